@@ -558,16 +558,15 @@ int orth_linear_xent(const orth_linear_xent_args* args, float* loss, float* lse,
  * Its vector-Jacobian product: with dz_rc = scale grad_loss[r] (exp(z_rc -
  * lse[r]) - [c is r's target]), grad_x = dz W and grad_w = dz^T x (either may
  * be NULL).  The classes are taken in pieces: the workspace holds dz of one
- * piece, in dtype (bfloat16: rounded once before its two products, without the
- * mantissa of the first rows' scale grad_loss, which multiplies their fp32 sums:
- * a grad_loss that all rows share costs nothing in precision), with several
- * pieces grad_x's fp32 sum, and a copy of x.  (bfloat16 heads of many
+ * piece, in fp32 or for bfloat16 operands as two bfloat16 pieces (16 bits, so
+ * that the gradients are off by little more than their own rounding), with
+ * several pieces grad_x's fp32 sum, and a copy of x.  (bfloat16 heads of many
  * rows whose rows of W are not 16-byte aligned take a padded copy of W too,
  * here and in orth_linear_xent.)  Rows without a target get zeros and add
  * nothing to grad_w, whatever x holds there (NaN included).  lse: what
  * orth_linear_xent gave; grad_loss: device, fp32, dL/d(loss[r]).
  * Both calls can be captured.  Errors: ORTH_EINVAL for NULL pointers, sizes
- * out of range, leading dimensions below the columns, a non-finite scale,
+ * out of range (bfloat16 gradients: more than 2^29 rows), leading dimensions below the columns, a non-finite scale,
  * piece < 0, an unknown dtype, or gradients that overlap an input or each
  * other.
  */

@@ -18,7 +18,8 @@ enum RowsEpi : int32_t {
   ROWS_LSE = 2,     // running maximum and sum of exponentials of scale * acc over the tile's columns
   ROWS_SLICE = 4,   // fp32 sums of a slice of kslice k's, which rows_join adds up (grouped along M: one
                     // group, slices along the grid's y)
-  ROWS_DZ = 3       // C = scale * grad_loss * (exp(scale * acc - lse) - [column is the target])
+  ROWS_DZ = 3       // C = scale * grad_loss * (exp(scale * acc - lse) - [column is the target]), in bf16 as
+                    // two pieces (c_low)
 };
 
 // Slices' sums (M x N each, one after the other) to be added up in order,
@@ -65,32 +66,17 @@ struct RowsProd {
   // tiles', which spares a launch (5 us each in a chain of short ones)
   void* copy;                // ROWS_DZ of the kernel without staging: A's rows, zeros for those without a
   int32_t ld_copy;           // target and up to ld_copy columns (nullptr: none)
+  int32_t twice;             // ... each as rows 2 i and 2 i + 1
   RowsJoin join;             // grouped along K: an earlier launch's slices
-  const float* factor;       // of all sums (nullptr: none), on the device
-  float* factor_out;         // ROWS_DZ in bf16: where the factor that dz leaves out goes
+  // A bf16 dz is held as two pieces, the rounding of the value and of what that
+  // leaves (off by 2^-16 of a value at most; with one piece, off by 2^-8, the
+  // gradients were 1.9e-3 off in the 2-norm where their own rounding is
+  // 1.7e-3).  Row r's lie in rows 2 r and 2 r + 1, so that its products are those
+  // of twice the rows: dW's k runs over both (x's rows twice each), dx's rows
+  // are added by pairs.
+  int32_t pairs;             // grouped along M, bf16, B k-major: 1: A's rows are such pairs, C has M / 2 rows
+  int64_t c_low;             // ROWS_DZ in bf16: elements from a value's first piece to its second
 };
-
-// ROWS_DZ in bf16: the factor F in [1, 2) that the stored dz leaves out and the
-// sums of its products are multiplied by, the mantissa of scale * grad_loss of
-// the first row (of the first 64) that has a target.  Where all rows share one
-// grad_loss, as in a mean, the targets' entries are then powers of two times
-// p - 1; with F in them each would be rounded by the same share of the constant
-// (8167 rows, 19056 classes: gradients off by 2.1e-3 from that alone, 2^-9 at
-// worst), which does not average out.
-__device__ __forceinline__ float dz_factor(const RowsProd& p, int lane) {
-  if (!p.factor_out) return 1.f;
-  bool ok = false;
-  float f = 0.f;
-  if (lane < p.rows) {
-    const int64_t t = ((const ORTH_GLOBAL int64_t*)p.targets)[lane];
-    f = gld_f32(p.grad_loss, lane) * p.scale;
-    ok = t >= 0 && t < p.classes && f != 0.f && f * 0.f == 0.f;
-  }
-  const unsigned long long has = __ballot(ok);
-  if (!has) return 1.f;
-  const uint32_t bits = __builtin_amdgcn_readlane(__float_as_uint(f), __ffsll(has) - 1);
-  return __uint_as_float((bits & 0x007fffffu) | 0x3f800000u);
-}
 
 // Group g's row range from the offsets, whatever they hold: each clamped to
 // [0, rows], and to the largest before it, so that ranges never overlap.
@@ -332,6 +318,16 @@ __device__ __forceinline__ bool rows_joined(const RowsJoin& p, int tid) {
   return true;
 }
 
+// What bf16 leaves of four values (nothing of one that it makes infinite).
+__device__ __forceinline__ float4 low4(float4 v) {
+  const uint32_t a = cvt2_bf16(v.x, v.y), b = cvt2_bf16(v.z, v.w);
+  auto rest = [](float x, uint32_t h) {
+    const float r = x - __uint_as_float(h);
+    return r * 0.f == 0.f ? r : 0.f;
+  };
+  return make_float4(rest(v.x, a << 16), rest(v.y, a & 0xffff0000u), rest(v.z, b << 16), rest(v.w, b & 0xffff0000u));
+}
+
 // One 4-column piece of a row of a finished tile: row i (of A and C), column
 // j, n columns left.
 template <int EPI>
@@ -353,10 +349,11 @@ __device__ __forceinline__ void rows_finish4(const RowsProd& p, int g, int64_t i
     else
       rows_store4(s, 0, ORTH_F32, u, n);
   } else if constexpr (EPI == ROWS_SLICE) {
-    rows_store4(p.slices, ((int64_t)g * p.M + i) * p.N + j, ORTH_F32, v, n);   // (g: the slice)
+    rows_store4(p.slices, ((int64_t)g * (p.M >> p.pairs) + i) * p.N + j, ORTH_F32, v, n);   // (g: the slice)
   } else {
     static_assert(EPI == ROWS_DZ);
     rows_store4(p.C, i * p.ldc + j, p.c_dtype, v, 4);
+    if (p.c_low) rows_store4(p.C, i * p.ldc + j + p.c_low, p.c_dtype, low4(v), 4);
   }
 }
 
@@ -374,7 +371,7 @@ __device__ __forceinline__ void rows_finish4(const RowsProd& p, int g, int64_t i
 typedef float orth_f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 
-template <int MI, int NI, int EPI>
+template <int MI, int NI, int EPI, bool PAIRS>   // PAIRS: p.pairs may be set
 struct RowsEpilogue {
   static constexpr int TN = NI * 32, NC = TN / 4;   // columns, 16-byte pieces of a row
   static constexpr int RQ = 64 / NC, NQ = 32 / RQ;  // rows of a pass of the wave, passes of a chunk
@@ -394,11 +391,6 @@ struct RowsEpilogue {
   }
   __device__ __forceinline__ void load_rows() {
     if constexpr (EPI == ROWS_DZ || EPI == ROWS_LSE) {
-      float factor = 1.f;
-      if constexpr (EPI == ROWS_DZ) {
-        factor = dz_factor(p, lane);
-        if (p.factor_out && ibase == 0 && jbase == 0 && lane == 0) gst_f32(p.factor_out, 0, factor);
-      }
 #pragma unroll
       for (int v = 0; v < RV; ++v) {
         const int r = v * 64 + lane;
@@ -408,7 +400,7 @@ struct RowsEpilogue {
           tcol[v] = t < 0 || t >= p.classes ? -2 : c >= 0 && c < TN ? (int)c : -1;
           if constexpr (EPI == ROWS_DZ) {
             lse[v] = gld_f32(p.lse, ibase + r);
-            gs[v] = gld_f32(p.grad_loss, ibase + r) * p.scale / factor;
+            gs[v] = gld_f32(p.grad_loss, ibase + r) * p.scale;
           }
         }
       }
@@ -487,16 +479,16 @@ struct RowsEpilogue {
     return make_float4(w[0], w[1], w[2], w[3]);
   }
 
-  // Whole blocks: four columns per lane, RQ rows per pass.
-  template <bool BF16>
+  // Whole blocks: four columns per lane, RQ rows (PAIR: of C) per pass.
+  template <bool BF16, bool PAIR>
   __device__ __forceinline__ void write_chunk(int mi) {
     const int lr = lane / NC, lc = (lane % NC) * 4;
     constexpr int ES = BF16 ? 2 : 4;
-    const int64_t row0 = ibase + mi * 32;
+    const int64_t row0 = (ibase + mi * 32) >> (PAIR ? 1 : 0);
     char* base;
     int64_t ld;
     if constexpr (EPI == ROWS_SLICE) {
-      base = reinterpret_cast<char*>(p.slices + ((int64_t)g * p.M + row0) * p.N + jbase);
+      base = reinterpret_cast<char*>(p.slices + ((int64_t)g * (PAIR ? p.M / 2 : p.M) + row0) * p.N + jbase);
       ld = p.N;
     } else if constexpr (EPI == ROWS_SUM) {
       base = static_cast<char*>(p.C) + (row0 * p.ldc + jbase) * ES;
@@ -507,11 +499,13 @@ struct RowsEpilogue {
     }
     const uint32_t off = (uint32_t)(lr * ld + lc) * ES;
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
+    for (int q = 0; q < (PAIR ? NQ / 2 : NQ); ++q) {
       const int r = q * RQ + lr;
-      const orth_f32x4 v = piece(r, lc);
+      const orth_f32x4 v = PAIR ? piece(2 * r, lc) + piece(2 * r + 1, lc) : piece(r, lc);
       float4 o = make_float4(v.x, v.y, v.z, v.w);
       if constexpr (EPI == ROWS_DZ) o = dz4(mi, r, lc, v);
+      if constexpr (EPI == ROWS_DZ && BF16)
+        rows_store4(base + ((int64_t)q * RQ * ld + p.c_low) * ES + off, 0, ORTH_BF16, low4(o), 4);
       if constexpr (EPI == ROWS_SUM) {
         if (p.add) {
           const orth_f32x4_a4 u = *(const ORTH_GLOBAL orth_f32x4_a4*)(p.sum + (row0 + r) * p.N + jbase + lc);
@@ -529,10 +523,12 @@ struct RowsEpilogue {
   __device__ __forceinline__ void edge_chunk(int mi) {
     const int ncols = (EPI == ROWS_DZ ? (p.N + 7) / 8 * 8 : p.N) - jbase;   // columns to write
     const int lr = lane / NC, lc = (lane % NC) * 4;
+    const int two = PAIRS ? p.pairs : 0;
 #pragma unroll 4
     for (int q = 0; q < NQ; ++q) {
+      if (q >= NQ >> two) break;
       const int r = q * RQ + lr;
-      const orth_f32x4 v = piece(r, lc);
+      const orth_f32x4 v = two ? piece(2 * r, lc) + piece(2 * r + 1, lc) : piece(r, lc);
       float4 o = make_float4(v.x, v.y, v.z, v.w);
       if constexpr (EPI == ROWS_DZ) {
         o = dz4(mi, r, lc, v);
@@ -540,10 +536,21 @@ struct RowsEpilogue {
         const int n = p.N - jbase - lc;
         o = make_float4(n > 0 ? o.x : 0.f, n > 1 ? o.y : 0.f, n > 2 ? o.z : 0.f, n > 3 ? o.w : 0.f);
       }
-      if (mi * 32 + r < mrows) rows_finish4<EPI>(p, g, ibase + mi * 32 + r, jbase + lc, o, ncols - lc);
+      if (mi * 32 + (r << two) < mrows)
+        rows_finish4<EPI>(p, g, ((ibase + mi * 32) >> two) + r, jbase + lc, o, ncols - lc);
     }
   }
 
+  template <bool BF16>
+  __device__ __forceinline__ void write(int mi) {
+    if constexpr (PAIRS) {
+      if (p.pairs) {
+        write_chunk<BF16, true>(mi);
+        return;
+      }
+    }
+    write_chunk<BF16, false>(mi);
+  }
   __device__ __forceinline__ void run(const orth_f32x16 (&acc)[MI][NI]) {
     load_rows();
     const int64_t ld = EPI == ROWS_SLICE ? p.N : p.ldc;
@@ -557,9 +564,9 @@ struct RowsEpilogue {
         if constexpr (EPI == ROWS_LSE)
           lse_chunk<true>(mi);
         else if (EPI != ROWS_SLICE && p.c_dtype == ORTH_BF16)
-          write_chunk<true>(mi);
+          write<true>(mi);
         else
-          write_chunk<false>(mi);
+          write<false>(mi);
       }
     } else {
 #pragma unroll
@@ -575,11 +582,11 @@ struct RowsEpilogue {
     }
   }
 };
-template <int MI, int NI, int EPI>
+template <int MI, int NI, int EPI, bool PAIRS>
 __device__ __forceinline__ void rows_epilogue(const RowsProd& p, int g, const orth_f32x16 (&acc)[MI][NI], float* buf,
                                               float* buf2, int64_t ibase, int jbase, int mrows, int block, int lane) {
   if (mrows <= 0) return;
-  RowsEpilogue<MI, NI, EPI> e{p, buf2, buf, ibase, g, jbase, mrows, block, lane, {}, {}, {}};
+  RowsEpilogue<MI, NI, EPI, PAIRS> e{p, buf2, buf, ibase, g, jbase, mrows, block, lane, {}, {}, {}};
   e.run(acc);
 }
 

@@ -7,13 +7,14 @@
 // each tile's columns to a maximum m and a sum of exp(z - m) per row, which the
 // join turns into lse = m + log sum, loss = lse - z_target (all fp32).  The
 // backward forms z again, a piece of the classes at a time, and from it dz =
-// scale grad_loss (exp(z - lse) - [target]), rounded once to the operands' type
-// (bf16: without the factor that dz_factor takes out) as the operand of dx = dz W
-// and dW = dz^T x.  Against kept logits that is a
-// third more products (8 N V d flop) for N V fewer values to hold.  4096 rows,
-// 2048 features, 50003 classes in bf16: loss 0.72, backward 2.27 ms, together 1125
-// TFLOP/s of these, bound by the products.  8 rows, 4096 features, 131072
-// classes: loss 171 us, W read at 6.3 TB/s.
+// scale grad_loss (exp(z - lse) - [target]), the operand of dx = dz W and dW =
+// dz^T x: in fp32, or for bf16 operands in two bf16 pieces, 16 bits, whose
+// products are twice as many (8 N V d flop; with the loss and the second z 12).
+// Against kept logits the second z costs 2 N V d for N V fewer values to hold.
+// 4096 rows, 2048 features, 50003 classes in bf16: loss 0.71, backward 3.52 ms,
+// together 1190 TFLOP/s of these, bound by the products (with dz in one bf16
+// piece the backward took 2.27).  8 rows, 4096 features, 131072 classes: loss 171
+// us, W read at 6.3 TB/s.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -202,11 +203,11 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* part, int 
 }
 
 // Rows of a matrix with zeros in the columns up to ldo; targets (may be
-// NULL): zeros for rows without one.
+// NULL): zeros for rows without one.  twice: row i as rows 2 i and 2 i + 1.
 // A thread moves 16 bytes from any alignment to an aligned place.
 template <typename V>
 __global__ __launch_bounds__(256) void pad_rows_kernel(const V* x, int64_t ld, V* out, int ldo, int rows,
-                                                       int cols, const int64_t* targets, int classes) {
+                                                       int cols, const int64_t* targets, int classes, int twice) {
   constexpr int L = 16 / sizeof(V);
   for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
     const int64_t t = targets ? targets[i] : 0;
@@ -224,20 +225,22 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const V* x, int64_t ld, V
       }
       orth_u32x4 v;
       __builtin_memcpy(&v, w, 16);
-      *(ORTH_GLOBAL orth_u32x4*)(out + i * ldo + c) = v;
+      V* to = out + (i << twice) * ldo + c;
+      *(ORTH_GLOBAL orth_u32x4*)to = v;
+      if (twice) *(ORTH_GLOBAL orth_u32x4*)(to + ldo) = v;
     }
   }
 }
 
 hipError_t launch_pad(const void* x, int64_t ld, void* out, int ldo, int rows, int cols, int dtype,
-                      const int64_t* targets, int classes, const char* name, hipStream_t s) {
+                      const int64_t* targets, int classes, int twice, const char* name, hipStream_t s) {
   timing_begin(name, s);
   if (dtype == ORTH_BF16)
     hipLaunchKernelGGL(pad_rows_kernel<uint16_t>, dim3((unsigned)std::min(rows, kMaxRowBlocks)), dim3(256), 0, s,
-                       static_cast<const uint16_t*>(x), ld, static_cast<uint16_t*>(out), ldo, rows, cols, targets, classes);
+                       static_cast<const uint16_t*>(x), ld, static_cast<uint16_t*>(out), ldo, rows, cols, targets, classes, twice);
   else
     hipLaunchKernelGGL(pad_rows_kernel<float>, dim3((unsigned)std::min(rows, kMaxRowBlocks)), dim3(256), 0, s, static_cast<const float*>(x), ld,
-                       static_cast<float*>(out), ldo, rows, cols, targets, classes);
+                       static_cast<float*>(out), ldo, rows, cols, targets, classes, twice);
   const hipError_t e = hipGetLastError();
   timing_end(name, s);
   return e;
@@ -383,6 +386,13 @@ struct XentPlan {
   int tile = 0, ldw = 0, ldx = 0;   // padded copies
   size_t off_part = 0, off_target = 0, off_w = 0, off_x = 0, total = 0;
 };
+int validate_xent_vjp(const orth_linear_xent_args* a) {
+  const int rc = validate_xent(a);
+  if (rc) return rc;
+  // (bf16: dz takes two rows each)
+  return a->dtype == ORTH_BF16 && a->rows > kMaxSize / 2 ? invalid("size too large") : (int)ORTH_OK;
+}
+
 // (ws: the workspace, or any aligned address to size it)
 XentPlan xent_plan(const orth_linear_xent_args* a, unsigned char* ws) {
   XentPlan P;
@@ -429,22 +439,24 @@ double rows_time(int dtype, int64_t M, int64_t N, int64_t K) {
 
 // The backward: x' (the rows with a target, padded to a multiple of 8
 // columns), dz of one piece of the classes, and with several pieces the sum
-// of dx in fp32.
+// of dx in fp32.  In bf16 dz takes two rows (RowsProd::pairs), x' too.
 struct XentVjpPlan {
+  int two = 0;                  // 1: of that
   int piece = 0, ldz = 0, ldx = 0, ldw = 0;   // ldw: W's padded copy, 0: none
   int slices = 1, kslice = 0, dx_tile = 0;   // of a piece's dx product
   GradPlan dw, dw_last;         // of a piece's dW and the last one's, which may be smaller
-  size_t off_x = 0, off_dz = 0, off_w = 0, off_sum = 0, off_factor = 0, off_slices = 0, total = 0;   // (dx's and dW's slices take turns)
+  size_t off_x = 0, off_dz = 0, off_w = 0, off_sum = 0, off_slices = 0, total = 0;   // (dx's and dW's slices take turns)
 };
 XentVjpPlan xent_vjp_plan(const orth_linear_xent_args* a) {
   XentVjpPlan P;
-  const int64_t es = esize(a->dtype), rows = std::max(a->rows, 1);
-  // pieces whose dz takes 256 MB at most, but of 4096 classes at least; of
-  // multiples of 256 down to half of that, the one whose products take the
-  // fewest rounds of tiles.  (4096 rows, 2048 features, 50003 classes: two
-  // pieces of 24576 are 6 whole rounds of dz's 256-tiles and 3 of dW's each, 851
-  // classes are left: 2.26 ms; pieces of 12288 2.41, of 25088 2.37, one of all
-  // 2.31)
+  P.two = a->dtype == ORTH_BF16 ? 1 : 0;
+  const int64_t es = esize(a->dtype), rows = std::max(a->rows, 1), held = rows << P.two;
+  // pieces whose dz takes 256 MB at most (bf16: each of its two pieces), but of
+  // 4096 classes at least; of multiples of 256 down to half of that, the one
+  // whose products take the fewest rounds of tiles.  (4096 rows, 2048 features,
+  // 50003 classes: two pieces of 24576 are 6 whole rounds of dz's 256-tiles and 3
+  // of dW's each, 851 classes are left: 3.52 ms; pieces of 12288 3.84, of 25088
+  // 3.75, one of all 3.75)
   int64_t piece = a->piece;
   if (!piece) {
     const int64_t most = std::max<int64_t>(4096, (256ll << 20) / (rows * es) / 256 * 256);
@@ -455,7 +467,7 @@ XentVjpPlan xent_vjp_plan(const orth_linear_xent_args* a) {
          p -= step) {
       const int64_t whole = a->classes / p, rest = a->classes % p;
       auto time = [&](int64_t n) {
-        return n ? rows_time(a->dtype, rows, n, a->features) + rows_time(a->dtype, n, a->features, rows) + 10 : 0.0;
+        return n ? rows_time(a->dtype, rows, n, a->features) + rows_time(a->dtype, n, a->features, held) + 10 : 0.0;
       };
       const double t = whole * time(p) + time(rest);
       if (!piece || t < best) {
@@ -469,22 +481,22 @@ XentVjpPlan xent_vjp_plan(const orth_linear_xent_args* a) {
   P.piece = (int)piece;
   P.ldz = (int)((piece + 7) / 8 * 8);
   P.ldx = (a->features + 7) / 8 * 8;
-  P.off_dz = align_up((size_t)a->rows * P.ldx * es);
-  P.off_w = P.off_dz + align_up((size_t)a->rows * P.ldz * es);
+  P.off_dz = align_up((size_t)held * P.ldx * es);
+  P.off_w = P.off_dz + align_up((size_t)held * P.ldz * es);
   P.ldw = padded(a, a->w, a->ld_w);
   P.off_sum = P.off_w + (P.ldw ? align_up((size_t)a->classes * P.ldw * es) : 0);
   const size_t sum = align_up((size_t)a->rows * a->features * 4);
-  P.off_factor = P.off_sum + (piece < a->classes ? sum : 0);
-  P.off_slices = P.off_factor + kAlign;
+  P.off_slices = P.off_sum + (piece < a->classes ? sum : 0);
   // dx has few tiles and a long k: whole, or its k in slices on staged tiles or,
   // from few rows, on the kernel without staging, by the times (us) that they
   // take per round of workgroups and k, and to join.  Measured (us, dz and dx of
-  // 93718 classes and 1344 features in bf16, whole tiles or slices without
-  // staging / the slices this chooses): 128 rows 241 / 137, 512 rows 954 / 326, 2048
-  // rows 1581 / 1198; fp32, 128 rows 579 / 458.
+  // 93718 classes and 1344 features, whole tiles or slices without staging / the
+  // slices this chooses): fp32, 128 rows 579 / 458; bf16 with dz in one piece 128
+  // rows 241 / 137, 512 rows 954 / 326, 2048 rows 1581 / 1200 (in two, with what
+  // this chooses: 173, 463, 1855).
   RowsProd d{};
   d.groups = 1;
-  d.rows = d.M = a->rows;
+  d.rows = d.M = (int)held;
   d.N = a->features;
   d.lda = P.ldz;
   d.ldb = P.ldw ? P.ldw : a->ld_w;
@@ -521,7 +533,7 @@ XentVjpPlan xent_vjp_plan(const orth_linear_xent_args* a) {
   consider(32, n, tiles * n / 512 * (f32 ? 0.01 : 0.0045), 12);
   RowsProd w{};
   w.groups = 1;
-  w.rows = w.K = a->rows;
+  w.rows = w.K = (int)held;
   w.M = P.piece;
   w.N = a->features;
   w.lda = P.ldz;
@@ -568,9 +580,9 @@ int orth_linear_xent(const orth_linear_xent_args* a, float* loss, float* lse, vo
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t pe = hipSuccess;
   if (P.ldw)
-    pe = launch_pad(a->w, a->ld_w, ws + P.off_w, P.ldw, a->classes, a->features, a->dtype, nullptr, 1, "xent_pad", s);
+    pe = launch_pad(a->w, a->ld_w, ws + P.off_w, P.ldw, a->classes, a->features, a->dtype, nullptr, 1, 0, "xent_pad", s);
   if (P.ldx && pe == hipSuccess)
-    pe = launch_pad(a->x, a->ld_x, ws + P.off_x, P.ldx, a->rows, a->features, a->dtype, nullptr, 1, "xent_pad", s);
+    pe = launch_pad(a->x, a->ld_x, ws + P.off_x, P.ldx, a->rows, a->features, a->dtype, nullptr, 1, 0, "xent_pad", s);
   rc = hip_check(pe != hipSuccess ? pe : launch(P.logits, a->dtype, false, false, ROWS_LSE, P.tile, "xent_logits", s), "orth_linear_xent");
   if (rc) return rc;
   timing_begin("xent_join", s);
@@ -587,7 +599,7 @@ int orth_linear_xent(const orth_linear_xent_args* a, float* loss, float* lse, vo
 
 int orth_linear_xent_vjp_workspace_size(const orth_linear_xent_args* a, size_t* bytes) {
   if (!bytes) return invalid("bytes is NULL");
-  const int rc = validate_xent(a);
+  const int rc = validate_xent_vjp(a);
   if (rc) return rc;
   *bytes = a->rows == 0 ? 0 : xent_vjp_plan(a).total;
   return ORTH_OK;
@@ -596,7 +608,7 @@ int orth_linear_xent_vjp_workspace_size(const orth_linear_xent_args* a, size_t* 
 int orth_linear_xent_vjp(const orth_linear_xent_args* a, const float* lse, const float* grad_loss, void* grad_x,
                          int64_t ld_grad_x, void* grad_w, int64_t ld_grad_w, void* workspace, size_t workspace_bytes,
                          void* stream) {
-  int rc = validate_xent(a);
+  int rc = validate_xent_vjp(a);
   if (rc) return rc;
   if ((a->rows > 0 && (!lse || !grad_loss)) || (!grad_x && !grad_w)) return invalid("NULL data pointer");
   if ((grad_x && ld_grad_x < a->features) || (grad_w && ld_grad_w < a->features))
@@ -650,7 +662,7 @@ int orth_linear_xent_vjp(const orth_linear_xent_args* a, const float* lse, const
   void* x = ws;
   void* dz = ws + P.off_dz;
   float* sum = reinterpret_cast<float*>(ws + P.off_sum);
-  float* factor = a->dtype == ORTH_BF16 ? reinterpret_cast<float*>(ws + P.off_factor) : nullptr;
+  const int held = a->rows << P.two;
   struct Step {
     RowsProd p;
     bool at, bt;
@@ -672,22 +684,24 @@ int orth_linear_xent_vjp(const orth_linear_xent_args* a, const float* lse, const
     const char* w = (P.ldw ? reinterpret_cast<const char*>(ws + P.off_w) : static_cast<const char*>(a->w)) + c0 * ldw * es;
     int k = 0;
     const bool first = along && c0 == 0, own = first || !copy;
-    RowsProd z = product(own ? a->x : x, own ? a->ld_x : P.ldx, w, ldw, a->rows, n, a->features);
+    RowsProd z = product(own ? a->x : x, own ? a->ld_x : (int64_t)P.ldx << P.two, w, ldw, a->rows, n, a->features);
     z.copy = first ? x : nullptr;
     z.ld_copy = P.ldx;
+    z.twice = P.two;
     z.C = dz;
-    z.ldc = P.ldz;
+    z.ldc = (int64_t)P.ldz << P.two;
+    z.c_low = P.two ? P.ldz : 0;
     z.col0 = c0;
     z.classes = a->classes;
     z.scale = a->scale;
     z.targets = a->targets;
     z.lse = lse;
     z.grad_loss = grad_loss;
-    z.factor_out = factor;
     st[k++] = {z, false, false, ROWS_DZ, first ? 32 : tile_of(z, a->dtype, false, false), "xent_dz"};
     RowsJoin join{};
     if (grad_x) {
-      RowsProd d = product(dz, P.ldz, w, ldw, a->rows, a->features, n);
+      RowsProd d = product(dz, P.ldz, w, ldw, held, a->features, n);
+      d.pairs = P.two;
       d.b_pad8 = P.ldw ? 1 : 0;
       d.C = grad_x;
       d.ldc = ld_grad_x;
@@ -697,17 +711,15 @@ int orth_linear_xent_vjp(const orth_linear_xent_args* a, const float* lse, const
       d.last = c0 + n >= a->classes;
       d.kslice = P.kslice;
       d.slices = reinterpret_cast<float*>(ws + P.off_slices);
-      d.factor = factor;
       if (P.slices > 1)
-        join = {d.slices, d.sum, d.C, d.ldc, d.M, d.N, (n + P.kslice - 1) / P.kslice, d.add, d.last, d.c_dtype};
+        join = {d.slices, d.sum, d.C, d.ldc, a->rows, d.N, (n + P.kslice - 1) / P.kslice, d.add, d.last, d.c_dtype};
       st[k++] = {d, false, true, P.slices > 1 ? (int)ROWS_SLICE : one ? (int)ROWS_STORE : (int)ROWS_SUM, P.dx_tile,
                  "xent_grad_x"};
     }
     if (grad_w) {
-      RowsProd d = product(dz, P.ldz, x, P.ldx, a->rows, a->features, a->rows);
+      RowsProd d = product(dz, P.ldz, x, P.ldx, held, a->features, held);
       d.M = n;
       d.a_pad8 = d.b_pad8 = 1;
-      d.factor = factor;
       d.C = static_cast<char*>(grad_w) + (int64_t)c0 * ld_grad_w * es;
       d.ldc = ld_grad_w;
       const GradPlan& g = c0 + n >= a->classes ? P.dw_last : P.dw;
@@ -725,9 +737,9 @@ int orth_linear_xent_vjp(const orth_linear_xent_args* a, const float* lse, const
     if ((st[i].at ? grad_blocks(st[i].p, a->dtype, P.piece >= a->classes ? P.dw_last : P.dw) : rows_blocks(st[i].p, false, st[i].tile)) > kMaxBlocks) return invalid("rows x piece too large");
   hipError_t e = hipSuccess;
   if (copy && !along)
-    e = launch_pad(a->x, a->ld_x, x, P.ldx, a->rows, a->features, a->dtype, a->targets, a->classes, "xent_rows", s);
+    e = launch_pad(a->x, a->ld_x, x, P.ldx, a->rows, a->features, a->dtype, a->targets, a->classes, P.two, "xent_rows", s);
   if (P.ldw && e == hipSuccess)
-    e = launch_pad(a->w, a->ld_w, ws + P.off_w, P.ldw, a->classes, a->features, a->dtype, nullptr, 1, "xent_pad", s);
+    e = launch_pad(a->w, a->ld_w, ws + P.off_w, P.ldw, a->classes, a->features, a->dtype, nullptr, 1, 0, "xent_pad", s);
   for (int c0 = 0; c0 < a->classes && e == hipSuccess; c0 += P.piece) {
     const int k = steps_of(c0, st);
     for (int i = 0; i < k && e == hipSuccess; ++i) {

@@ -97,9 +97,6 @@ __device__ __forceinline__ void tile_body(const RowsProd& p, const TileWork& w, 
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
 
-  constexpr bool SUMS = EPI == ROWS_STORE || EPI == ROWS_SUM || EPI == ROWS_SLICE;
-  float factor = 1.f;   // (here, as a load behind the loop would be waited for)
-  if (SUMS && p.factor) factor = gld_f32(p.factor, 0);
   const int K = w.K, kmain = DMA ? K / BK * BK : 0;
   if constexpr (DMA)
     kloop<BM, BN, WM, WN, AT, BT, false, true, BAUX>(acc, w.A, p.lda, w.B, p.ldb, 0, kmain, l.a0, l.b0, l.a1, l.b1, l.x, wave,
@@ -156,25 +153,21 @@ __device__ __forceinline__ void tile_body(const RowsProd& p, const TileWork& w, 
     }
     __syncthreads();
   }
-  if (SUMS && p.factor) {
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-      for (int ni = 0; ni < NI; ++ni) acc[mi][ni] *= factor;
-  }
   // the waves' staging buffers, 32 rows of TN floats each: two fit the stage
   // that a wave takes (half a 256-tile has the stages of a whole one)
   constexpr int CH = 32 * T::TN * 2;
   uint16_t* at = wave == 0 ? l.a0 : wave == 1 ? l.b0 : wave == 2 ? l.a1 : l.b1;
   float* buf = reinterpret_cast<float*>(at);
   float* buf2 = reinterpret_cast<float*>(at + CH);
-  rows_epilogue<MI, NI, EPI>(p, w.g, acc, buf, buf2, w.i0 + wm * T::TM, w.j0 + wn * T::TN, w.mrows - wm * T::TM,
+  rows_epilogue<MI, NI, EPI, !AT && BT>(p, w.g, acc, buf, buf2, w.i0 + wm * T::TM, w.j0 + wn * T::TN, w.mrows - wm * T::TM,
                              w.col * WN + wn, lane);
 }
 
-// BAUX: cache policy of B's loads.
+// BAUX: cache policy of B's loads.  Without DMA the registers are held to what
+// leaves a unit two workgroups (us, one / two: 8000 rows, 4 x 2003 x 1333 112 / 83,
+// transposed 112 / 97, 1500 x 777 x 513 19.5 / 20.3).
 template <int BM, bool AT, bool BT, int EPI, bool DMA, int BAUX = 0>
-__global__ __launch_bounds__(kThreads, 1) void rows_bf16_kernel(const RowsProd p) {
+__global__ __launch_bounds__(kThreads, DMA ? 1 : 2) void rows_bf16_kernel(const RowsProd p) {
   constexpr int BN = BM, BK = 64;
   __shared__ __attribute__((aligned(1024))) uint16_t sA0[BM * BK];
   __shared__ __attribute__((aligned(1024))) uint16_t sB0[BN * BK];

@@ -83,8 +83,9 @@ __device__ __forceinline__ void split8(const uint4 (&v)[2], uint4 (&p)[3]) {
   for (int i = 0; i < 3; ++i) p[i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
 }
 
-// ROWS_DZ: rows of A into the copy, zeros for those without a target, eight
-// rows a workgroup.  16 bytes from any alignment to an aligned place.
+// ROWS_DZ: rows of A into the copy (p.twice: two rows each), zeros for those
+// without a target, eight rows a workgroup.  16 bytes from any alignment to an
+// aligned place.
 constexpr int kCopyRows = 8;
 template <int DT>
 __device__ __forceinline__ void copy_rows(const RowsProd& p, int block, int tid, int threads) {
@@ -108,7 +109,9 @@ __device__ __forceinline__ void copy_rows(const RowsProd& p, int block, int tid,
           if (c + e < p.K) w[e * ES / 4] |= ES == 2 ? (uint32_t)gld_u16(from, e) << (e % 2 * 16) : gld_u32(from, e);
         v = orth_u32x4{w[0], w[1], w[2], w[3]};
       }
-      *(ORTH_GLOBAL orth_u32x4*)(static_cast<char*>(p.copy) + (i * p.ld_copy + c) * ES) = v;
+      char* to = static_cast<char*>(p.copy) + ((i << p.twice) * p.ld_copy + c) * ES;
+      *(ORTH_GLOBAL orth_u32x4*)to = v;
+      if (p.twice) *(ORTH_GLOBAL orth_u32x4*)(to + (int64_t)p.ld_copy * ES) = v;
     }
   }
 }
@@ -261,13 +264,15 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
   };
   put(wave);
   __syncthreads();
-  // four columns of a row per thread, the first 256 threads
+  // four columns of a row per thread, the first 256 threads (the first 128
+  // where rows are added by pairs)
   const int row = tid >> 3, c4 = tid & 7;
+  const int two = DT == ORTH_BF16 && BT ? p.pairs : 0;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   auto add = [&](int n) {
-    v = sums[0][row][c4];
-    for (int w = 1; w < n; ++w) {
-      const float4 u = sums[w][row][c4];
+    v = sums[0][row << two & 31][c4];
+    for (int w = 1; w < n << two; ++w) {
+      const float4 u = sums[w >> two][((row << two) + (w & two)) & 31][c4];
       v.x += u.x;
       v.y += u.y;
       v.z += u.z;
@@ -311,14 +316,6 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
     }
   }
   if (tid >= 256) return;
-  float factor = 1.f;   // (ROWS_DZ: left out; others: of the sums)
-  if constexpr (EPI == ROWS_DZ) {
-    factor = dz_factor(p, lane);
-    if (p.factor_out && i0 == 0 && j0 == 0 && tid == 0) gst_f32(p.factor_out, 0, factor);
-  } else if (EPI != ROWS_LSE && p.factor) {
-    factor = gld_f32(p.factor, 0);
-    v = make_float4(v.x * factor, v.y * factor, v.z * factor, v.w * factor);
-  }
   if constexpr (EPI == ROWS_LSE) {
     float e[4] = {v.x, v.y, v.z, v.w};
     float top = -INFINITY;
@@ -344,11 +341,11 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
       const int64_t at = ((const ORTH_GLOBAL int64_t*)p.targets)[i] - p.col0 - j0 - c4 * 4;
       if (at >= 0 && at < 4 && c4 * 4 + at < ncols) gst_f32(p.ztarget, i, at == 0 ? e[0] : at == 1 ? e[1] : at == 2 ? e[2] : e[3]);
     }
-  } else if (row < mrows) {
+  } else if (row << two < mrows) {
     const int left = (EPI == ROWS_DZ ? (p.N + 7) / 8 * 8 : p.N) - j0;
     if constexpr (EPI == ROWS_DZ) {
       const int64_t i = i0 + row, t = ((const ORTH_GLOBAL int64_t*)p.targets)[i];
-      const float l = gld_f32(p.lse, i), f = gld_f32(p.grad_loss, i) * p.scale / factor;
+      const float l = gld_f32(p.lse, i), f = gld_f32(p.grad_loss, i) * p.scale;
       float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -360,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
       }
       v = make_float4(e[0], e[1], e[2], e[3]);
     }
-    rows_finish4<EPI>(p, EPI == ROWS_SLICE ? (int)blockIdx.y : t.g, i0 + row, j0 + c4 * 4, v, left - c4 * 4);
+    rows_finish4<EPI>(p, EPI == ROWS_SLICE ? (int)blockIdx.y : t.g, (i0 >> two) + row, j0 + c4 * 4, v, left - c4 * 4);
   }
 }
 

@@ -325,7 +325,7 @@ __global__ __launch_bounds__(BM == 64 ? 256 : 512, 2) void rows_f32_kernel(const
     }
   }
   constexpr int TM = BM / WM, TN = BM / WN;
-  rows_epilogue<MI, NI, EPI>(p, g, acc[0], reinterpret_cast<float*>(smem) + wave * (64 * TN),
+  rows_epilogue<MI, NI, EPI, false>(p, g, acc[0], reinterpret_cast<float*>(smem) + wave * (64 * TN),
                              reinterpret_cast<float*>(smem) + wave * (64 * TN) + 32 * TN, i0 + wm * TM,
                              tj * BM + wn * TN, side[0].lim - wm * TM, tj * WN + wn, lane);
 }

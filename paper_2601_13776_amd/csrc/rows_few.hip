@@ -139,8 +139,6 @@ __global__ __launch_bounds__(256, RB == 1 ? 3 : 2) void rows_outer_kernel(const 
   const char* A = static_cast<const char*>(p.A) + (range.start + 8 * h) * p.lda * ES;
   const char* B = static_cast<const char*>(p.B) + ((range.start + 8 * h) * p.ldb + j) * ES;
   const int rows = range.end - range.start;
-  float factor = 1.f;
-  if (p.factor) factor = gld_f32(p.factor, 0);
   FewA<DT> a;
   FewB<DT> b;
   a.load(A + (int64_t)min(i0 + r, p.M - 1) * ES, p.lda, 8 * h, rows);
@@ -157,10 +155,6 @@ __global__ __launch_bounds__(256, RB == 1 ? 3 : 2) void rows_outer_kernel(const 
     if (q + 1 < RB) {
       a.load(A + (int64_t)min(i0 + 128 + r, p.M - 1) * ES, p.lda, 8 * h, rows);
       if (rows > 16) b.load(B, p.ldb, 8 * h, rows, left);
-    }
-    if (p.factor) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] *= factor;
     }
     const int64_t base = (p.offsets ? g * p.gc : 0) + j;
 #pragma unroll

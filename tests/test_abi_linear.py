@@ -182,3 +182,16 @@ def test_binding_refusals():
         orth.orth_grad_list([x], [x, x])
     with pytest.raises(ValueError):
         orth.orth_grad_clip_batched([x], 1.0, norm_given=True)
+
+
+def test_vjp_rows(L):
+    """bf16 gradients hold dz in two rows each: up to 2^29 rows; the loss and
+    fp32 gradients 2^30."""
+    n = ctypes.c_size_t()
+    most = 2 ** 30
+    for dtype, rows, want in ((1, most // 2, OK), (1, most // 2 + 1, EINVAL), (0, most, OK)):
+        a = ctypes.byref(xent(dtype=dtype, rows=rows))
+        assert L.orth_linear_xent_vjp_workspace_size(a, ctypes.byref(n)) == want
+        assert L.orth_linear_xent_workspace_size(a, ctypes.byref(n)) == OK
+        if want != OK:
+            assert L.orth_linear_xent_vjp(a, 1 << 45, 2 << 45, 5 << 45, 64, 6 << 45, 64, 1 << 50, 1 << 40, None) == want
