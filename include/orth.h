@@ -488,7 +488,8 @@ typedef struct {
                               [offsets[g], offsets[g+1]) belong to matrix g.
                               NULL with groups == 1: every row */
   int32_t rows;            /* 0 .. 2^30; x and y may be NULL if 0 */
-  int32_t groups, in_features, out_features;   /* >= 1 (sizes up to 2^30) */
+  int32_t groups, in_features, out_features;   /* >= 1, up to 2^30; groups up to 2^20,
+                              as every workgroup reads all offsets */
   int64_t ld_x, ld_w, stride_w, ld_y;          /* stride_w: ignored if groups == 1; 0: every
                                                   group applies the same matrix */
   int32_t dtype;           /* orth_dtype */

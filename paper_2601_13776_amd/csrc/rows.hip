@@ -53,6 +53,9 @@ int64_t esize(int dtype) { return dtype == ORTH_BF16 ? 2 : 4; }
 constexpr int64_t kMaxBlocks = (1 << 23) - 1;   // of up to 512 threads: a grid holds less than 2^32
 constexpr int kMaxRowBlocks = 1 << 20;          // of kernels that take rows in turn
 constexpr int kMaxSize = 1 << 30;   // of every extent: sums of two stay within 32 bits
+// Every workgroup reads all offsets, 64 at a time with 32-bit counters (which
+// 2^31 groups overflow): 0.6 ms of 2^16 groups, 9 ms of the most.
+constexpr int kMaxGroups = 1 << 20;
 
 // Whether [a, a + n) and [b, b + m) share a byte.
 bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
@@ -258,6 +261,7 @@ int validate_linear(const orth_linear_args* a, bool grad) {
     return invalid("rows must be >= 0, groups, in_features and out_features >= 1");
   if (a->rows > kMaxSize || a->in_features > kMaxSize || a->out_features > kMaxSize)
     return invalid("size too large");
+  if (a->groups > kMaxGroups) return invalid("too many groups");
   if (!a->offsets && a->groups != 1) return invalid("offsets is NULL with several groups");
   const int64_t cx = grad || !a->transposed ? a->in_features : a->out_features;
   const int64_t cy = grad || !a->transposed ? a->out_features : a->in_features;

@@ -195,3 +195,18 @@ def test_vjp_rows(L):
         assert L.orth_linear_xent_workspace_size(a, ctypes.byref(n)) == OK
         if want != OK:
             assert L.orth_linear_xent_vjp(a, 1 << 45, 2 << 45, 5 << 45, 64, 6 << 45, 64, 1 << 50, 1 << 40, None) == want
+
+
+@pytest.mark.parametrize("groups", [2 ** 20 + 1, 2 ** 30, BIG])
+def test_too_many_groups(L, groups):
+    """The device counts groups in 32 bits, 64 offsets at a time in every
+    workgroup: more groups than that can be read in milliseconds are refused
+    (with one matrix for all, which no bound on stride_w reaches)."""
+    n = ctypes.c_size_t()
+    a = ctypes.byref(linear(groups=groups, stride_w=0))
+    assert L.orth_linear_apply(a, None) == EINVAL
+    a = ctypes.byref(linear(groups=groups))
+    assert L.orth_linear_grad_weight_workspace_size(a, ctypes.byref(n)) == EINVAL
+    assert L.orth_linear_grad_weight(a, 1 << 50, 1 << 40, None) == EINVAL
+    a = ctypes.byref(linear(groups=2 ** 20))
+    assert L.orth_linear_grad_weight_workspace_size(a, ctypes.byref(n)) == OK
