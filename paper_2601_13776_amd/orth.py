@@ -742,7 +742,12 @@ class orth_grad_list:
     clipped ones; default: in place), for orth_grad_norm_batched and
     orth_grad_clip_batched.  Tensors of up to two dimensions with unit column
     stride, or contiguous ones of any; float32 and bfloat16 may be mixed.  A
-    program that keeps its gradients' buffers keeps this list with them."""
+    program that keeps its gradients' buffers keeps this list with them: its
+    descriptors are made once (8 us a tensor).  The list holds the tensors'
+    memory, and every call looks whether each tensor is still where it was (50
+    ns each) and makes the descriptors again where one is not, its .data
+    replaced or resized past its storage.  A tensor that changes its shape where
+    it is needs refresh()."""
 
     def __init__(self, grads, outs=None):
         outs = grads if outs is None else outs
@@ -751,9 +756,23 @@ class orth_grad_list:
         if not grads:
             raise ValueError("the list must hold at least one tensor")
         self.tensors = (list(grads), list(outs))
+        self._every = [*grads, *(o for g, o in zip(grads, outs) if o is not g)]
+        self.refresh()
+
+    def _current(self):
+        if list(map(torch.Tensor.data_ptr, self._every)) != self._at:
+            self.refresh()
+        return self
+
+    def refresh(self):
+        """Makes the descriptors again from the tensors as they are now."""
+        grads, outs = self.tensors
+        self._at = None   # (nothing is taken for read if this raises)
         self.device = grads[0].device
         if any(t.device != self.device for t in (*grads, *outs)) or self.device.type != "cuda":
             raise ValueError("all tensors must be on one GPU")
+        # (what the descriptors point to stays allocated while they do)
+        self._memory = list(map(torch.Tensor.untyped_storage, self._every))
         descs = []
         for g, o in zip(grads, outs):
             if g.shape != o.shape or g.dtype != o.dtype:
@@ -767,6 +786,7 @@ class orth_grad_list:
         _check(lib().orth_grad_norm_workspace_size(self.array, len(descs), ctypes.byref(n)),
                "orth_grad_norm_workspace_size")
         self.workspace_bytes = n.value
+        self._at = list(map(torch.Tensor.data_ptr, self._every))
 
     @staticmethod
     def _matrices(g, o):
@@ -777,11 +797,15 @@ class orth_grad_list:
             return [(g[i:i + most].view(1, -1), o[i:i + most].view(1, -1)) for i in range(0, max(g.numel(), 1), most)]
         if g.dim() > 2:
             raise ValueError("gradients of more than two dimensions must be contiguous")
+        for t in (g, o):   # (a view, as above, says so by itself)
+            last = t.storage_offset() + sum((n - 1) * k for n, k in zip(t.shape, t.stride()))
+            if t.numel() and (last + 1) * t.element_size() > t.untyped_storage().nbytes():
+                raise RuntimeError("a gradient's storage does not hold it")
         return [(g, o) if g.dim() == 2 else (g.unsqueeze(1), o.unsqueeze(1))]
 
 
 def _as_list(grads):
-    return grads if isinstance(grads, orth_grad_list) else orth_grad_list(grads)
+    return grads._current() if isinstance(grads, orth_grad_list) else orth_grad_list(grads)
 
 
 def _norm_call(fn, where, lst, norm, workspace, stream, *opts):

@@ -152,3 +152,56 @@ def test_captured_clip_and_long_lists():
         graph.replay()
         torch.cuda.synchronize()
         check_clip(grads, lst.tensors[1], norm, 1.0)
+
+
+@pytest.mark.parametrize("apart", [False, True])
+def test_kept_list_follows_its_tensors(apart):
+    """A kept list whose tensors got other memory since it was made: replaced
+    .data, resized beyond their storage and within it, storage given up."""
+    print(f"[grad clip moved] {apart}", flush=True)
+    grads = [rand((64, 30), 1, F32), rand((200,), 2, BF16), rand((9, 9), 3, F32)]
+    outs = [torch.empty_like(g) for g in grads] if apart else None
+    lst = orth.orth_grad_list(grads, outs)
+    kept = [g.clone() for g in grads]
+
+    def check():
+        before = [g.clone() for g in grads]
+        norm = orth.orth_grad_clip_batched(lst, 0.5)
+        check_clip(before, outs if apart else grads, norm, 0.5)
+        assert torch.equal(orth.orth_grad_norm_batched(before), norm)
+
+    check()
+    old = grads[0].data
+    grads[0].data = rand((64, 30), 4, F32)
+    was = old.clone()
+    check()
+    assert torch.equal(old, was)               # nothing is written where the tensor was
+    grads[1].data = rand((70, 80), 5, BF16)    # another shape
+    if apart:
+        with pytest.raises(ValueError):
+            orth.orth_grad_clip_batched(lst, 0.5)
+        with pytest.raises(ValueError):        # (and again: the list is not taken for read)
+            orth.orth_grad_norm_batched(lst)
+        outs[1].data = torch.empty(70, 80, dtype=BF16, device=DEV)
+    check()
+    for size in ((300, 300), (2, 3)):          # past the storage, within it
+        for t in (grads[2], *(outs[2:] if apart else ())):
+            t.resize_(size)
+        grads[2].copy_(rand(size, 6, F32))
+        if size == (2, 3):
+            lst.refresh()                      # (where it was: the list cannot see it)
+        check()
+    if apart:
+        outs[0].data = torch.empty(64, 30, device=DEV)
+        check()
+    grads[0].untyped_storage().resize_(0)
+    with pytest.raises(RuntimeError):
+        orth.orth_grad_clip_batched(lst, 0.5)
+    grads[0].untyped_storage().resize_(64 * 30 * 4)
+    grads[0].copy_(kept[0])
+    check()
+    slices = [rand((40, 50), 7, F32)[:, 3:20]]   # (an address of 12 is no memory either)
+    kept_slices = orth.orth_grad_list(slices)
+    slices[0].untyped_storage().resize_(0)
+    with pytest.raises(RuntimeError):
+        orth.orth_grad_norm_batched(kept_slices)
