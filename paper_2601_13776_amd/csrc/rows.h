@@ -243,6 +243,10 @@ __device__ __forceinline__ RowsKTile rows_ktile(const RowsProd& p, int bm, int i
   return k;
 }
 
+// Orders results by size, zero behind the largest (2 |v| as bits, less 1): a
+// split product below small_key(kSplitLo) may lack low pieces of its operands.
+__device__ __forceinline__ uint32_t small_key(float v) { return (__float_as_uint(v) << 1) - 1; }
+
 // 16 or 8 bytes at any 2-byte aligned address
 typedef uint32_t orth_u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t orth_u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));

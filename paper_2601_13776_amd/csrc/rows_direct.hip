@@ -282,10 +282,9 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
   if (tid < 256) add(kWaves);
   if constexpr (DT == ORTH_F32) {
     // results that the split cannot give, from the tile's fp32 MFMA products:
-    // those that are not finite, or a thread's four if they are too small
-    const float top = fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
-    const float nan = fmaf(v.x, 0.f, v.y * 0.f) + fmaf(v.z, 0.f, v.w * 0.f);
-    const bool bad = tid < 256 && (!(nan == 0.f) || (top > 0.f && top < kSplitLo));
+    // those that are not finite or too small, each by itself
+    auto fails = [](float r) { return !(r * 0.f == 0.f) || small_key(r) < small_key(kSplitLo); };
+    const bool bad = tid < 256 && (fails(v.x) || fails(v.y) || fails(v.z) || fails(v.w));
     if (__syncthreads_or(bad)) {
       if (wave == 0) {
         acc = f32x16{};
@@ -307,11 +306,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
       if (bad) {
         const float4 o = v;
         add(1);
-        const bool all = top < kSplitLo;
-        if (!all && o.x * 0.f == 0.f) v.x = o.x;
-        if (!all && o.y * 0.f == 0.f) v.y = o.y;
-        if (!all && o.z * 0.f == 0.f) v.z = o.z;
-        if (!all && o.w * 0.f == 0.f) v.w = o.w;
+        if (!fails(o.x)) v.x = o.x;
+        if (!fails(o.y)) v.y = o.y;
+        if (!fails(o.z)) v.z = o.z;
+        if (!fails(o.w)) v.w = o.w;
       }
     }
   }

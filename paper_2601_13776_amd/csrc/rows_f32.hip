@@ -43,11 +43,9 @@ __device__ __forceinline__ void load4(const float* p, float* x) {
 // are so small (but not zero) that low pieces of their operands may have fallen
 // off the end of bfloat16's range.  Each is asked by itself (a lane's 16 are as
 // many rows), so that a row's results do not depend on what other rows hold.
-// (2 |v| as bits, less 1, which makes zero the largest.  Blocks computed again are
-// read value by value: a head's dW takes 4 times as long, 1190 us for 284 at 2000
-// rows, 264 features, 8000 classes, where most probabilities are below 2^-100 but
-// not zero in every row, logits of +-300.)
-__device__ __forceinline__ uint32_t small_key(float v) { return (__float_as_uint(v) << 1) - 1; }
+// Blocks computed again are read value by value: a head's dW takes 4 times as long,
+// 1190 us for 284 at 2000 rows, 264 features, 8000 classes, where most
+// probabilities are below 2^-100 but not zero in every row, logits of +-300.
 __device__ __forceinline__ bool any_failed(const f32x16& v) {
   uint32_t least = ~0u;
   float nan0 = 0.f, nan1 = 0.f;

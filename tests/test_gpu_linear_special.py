@@ -10,6 +10,7 @@ from test_gpu_linear import rand
 
 pytestmark = pytest.mark.gpu
 
+
 def tiny(shape, seed):
     """Values of either sign in [1, 2) 2^-118: their second bfloat16 pieces lie
     at the end of its normal range, their third ones past it."""
@@ -48,3 +49,17 @@ def test_tiny_rows_beside_ordinary_ones(n_out, transposed):
     gw = orth.orth_linear_grad_weight(gy, xs)
     assert torch.all(apart(gw, torch.mm(gy.double().t().contiguous(), xs.double()))
                      <= 1.5 * 2.0 ** -24 * (700 / 12) ** 0.5)
+
+
+@pytest.mark.parametrize("rows,k,n_out", [(20, 264, 90), (3, 1000, 77), (2000, 264, 3577)])
+def test_tiny_rows_of_a_matrix(rows, k, n_out):
+    """The same of outputs whose weights are that small beside the others', with
+    and without staging."""
+    print(f"[linear tiny weights] {rows} {k} {n_out}", flush=True)
+    x, w = rand((rows, k), 7, torch.float32, 16.0), rand((n_out, k), 8, torch.float32)
+    at = [0, 5, 6, 33, 76]
+    w[at] = tiny((5, k), 9)
+    y = orth.orth_linear_apply(x, w)
+    far = apart(y.t().contiguous(), torch.mm(w.double(), x.double().t()))
+    # (norms of a few rows only: twice for chance)
+    assert torch.all(far <= 2 * 2.0 ** -24 * (k / 12) ** 0.5), float(far.max())
