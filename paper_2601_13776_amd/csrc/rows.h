@@ -375,6 +375,11 @@ __device__ __forceinline__ void rows_finish4(const RowsProd& p, int g, int64_t i
 typedef float orth_f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 
+// What a sum of exponentials is relative to, by its largest value: 0 for an
+// infinite one, so that no difference of infinities is formed (every value -inf:
+// the sum is 0, one +inf: it is inf).
+__device__ __forceinline__ float lse_base(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
+
 template <int MI, int NI, int EPI, bool PAIRS>   // PAIRS: p.pairs may be set
 struct RowsEpilogue {
   static constexpr int TN = NI * 32, NC = TN / 4;   // columns, 16-byte pieces of a row
@@ -447,15 +452,14 @@ struct RowsEpilogue {
         top = fmaxf(top, v[q][k]);
       }
     }
-    // (every value -inf: nothing is added, and no difference of infinities formed)
-    const float from = top == -INFINITY ? 0.f : top;
+    const float from = lse_base(top);
     float sum = 0.f;
 #pragma unroll
     for (int q = 0; q < NC / 2; ++q)
 #pragma unroll
       for (int k = 0; k < 4; ++k) sum += __builtin_amdgcn_exp2f((v[q][k] - from) * kLog2e);
     const float otop = __shfl_xor(top, 32, 64), osum = __shfl_xor(sum, 32, 64);
-    const float m = fmaxf(top, otop), to = m == -INFINITY ? 0.f : m;
+    const float m = fmaxf(top, otop), to = lse_base(m);
     const float total = sum * __builtin_amdgcn_exp2f((top - to) * kLog2e) +
                         osum * __builtin_amdgcn_exp2f((otop - to) * kLog2e);
     const int tc = __shfl(tcol[mi / 2], (mi & 1) * 32 + r, 64) - c0;

@@ -174,14 +174,15 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* part, int 
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) m = fmaxf(m, v[u].x);
-      sum = sum == 0.f ? 0.f : sum * __expf(top - m);
+      const float from = lse_base(m);
+      sum = sum == 0.f ? 0.f : sum * __expf(top - from);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) sum += v[u].y == 0.f ? 0.f : v[u].y * __expf(v[u].x - m);
+      for (int u = 0; u < 8; ++u) sum += v[u].y == 0.f ? 0.f : v[u].y * __expf(v[u].x - from);
       top = m;
     }
     auto join = [](float& t, float& s, float ot, float os) {
-      const float m = fmaxf(t, ot);
-      s = (s == 0.f ? 0.f : s * __expf(t - m)) + (os == 0.f ? 0.f : os * __expf(ot - m));
+      const float m = fmaxf(t, ot), from = lse_base(m);
+      s = (s == 0.f ? 0.f : s * __expf(t - from)) + (os == 0.f ? 0.f : os * __expf(ot - from));
       t = m;
     };
 #pragma unroll

@@ -324,10 +324,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void rows_direct_kernel(const RowsP
     }
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float from = lse_base(top);
     float sum = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)   // (NaN - top is NaN; with every value -inf nothing is added)
-      sum += c4 * 4 + q < ncols && !(e[q] == -INFINITY) ? __builtin_amdgcn_exp2f((e[q] - top) * kLog2e) : 0.f;
+    for (int q = 0; q < 4; ++q) sum += c4 * 4 + q < ncols ? __builtin_amdgcn_exp2f((e[q] - from) * kLog2e) : 0.f;
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) sum += __shfl_xor(sum, d, 64);
     if (row < mrows) {

@@ -220,6 +220,28 @@ def test_classes_of_no_weight(dtype):
     assert torch.all((lse.double() - r_lse).abs() <= tol) and torch.all((loss.double() - r_loss).abs() <= tol)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,features,classes", [(5, 64, 300), (6, 128, 70000), (700, 264, 4001)])
+def test_infinite_logits(rows, features, classes, dtype):
+    """lse of a row with a logit of +inf is +inf, of -inf ones and +inf ones too;
+    all of -inf give -inf, and one NaN gives NaN.  The other rows are as without."""
+    print(f"[xent infinite logits] {rows} {features} {classes} {dtype}", flush=True)
+    dt = DT[dtype]
+    x, w = rand((rows, features), 29, dt), rand((classes, features), 30, dt, features ** -0.5)
+    w[:, 0] = w[:, 0].abs() + 2.0 ** -9
+    plain = orth.orth_linear_xent(x, w, torch.full((rows,), 3, device=DEV))
+    x[0, 0], x[1, 0], x[2, 1], x[3, 0], x[3, 1] = INF, -INF, INF, INF, NAN
+    t = torch.full((rows,), 3, device=DEV)
+    loss, lse = orth.orth_linear_xent(x, w, t)
+    z = torch.mm(x.double(), w.double().t().contiguous())
+    want = torch.logsumexp(z, 1)
+    assert want[0] == INF and want[1] == -INF and want[2] == INF and torch.isnan(want[3])
+    assert torch.equal(lse[:3].double(), want[:3]) and torch.isnan(lse[3])
+    assert torch.isnan(loss[0]) and torch.isnan(loss[1]) and torch.isnan(loss[3])       # inf - inf
+    assert loss[2] == INF if z[2, 3] == -INF else torch.isnan(loss[2])
+    assert torch.equal(lse[4:], plain[1][4:]) and torch.equal(loss[4:], plain[0][4:])
+
+
 @pytest.mark.parametrize("counts,n_in,n_out", [([2000, 100, 1500], 264, 3577), ([4096], 256, 4096), ([200, 0, 30, 9] * 60, 64, 136),
                                                ([700], 1000, 90), ([64] * 20, 90, 256)])
 def test_fp32_products_keep_24_bits(counts, n_in, n_out):
