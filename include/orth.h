@@ -581,8 +581,8 @@ typedef struct {
   const void* grad;      /* device, rows x cols, leading dim ld_grad */
   void* out;             /* device, rows x cols, leading dim ld_out: the clipped
                             gradient (ignored by orth_grad_norm_batched).  May
-                            equal grad (equal leading dims); no output may
-                            overlap another tensor */
+                            equal grad (equal leading dims) or be apart from
+                            it; no output may overlap another tensor */
   int32_t rows, cols;    /* >= 0; an empty tensor's pointers may be NULL */
   int64_t ld_grad, ld_out;
   int32_t dtype;         /* orth_dtype of both; a list may mix them */
@@ -607,8 +607,10 @@ typedef struct {
  * capturing stream).
  * Both use a workspace of orth_grad_norm_workspace_size.
  * Returns ORTH_EINVAL for n < 0, NULL pointers, negative sizes, leading
- * dimensions below the columns, an unknown dtype, in == out with differing
- * leading dims, two equal outputs, or options out of range.
+ * dimensions below the columns or past any memory, an unknown dtype, in ==
+ * out with differing leading dims, an output that shares a part of its
+ * gradient, two outputs that are equal or contiguous and overlap, or options
+ * out of range.
  */
 int orth_grad_norm_workspace_size(const orth_grad* grads, int32_t n, size_t* bytes);
 int orth_grad_norm_batched(const orth_grad* grads, int32_t n, float* norm, void* workspace,

@@ -378,6 +378,28 @@ __global__ __launch_bounds__(kThreads) void grad_norm_join_kernel(const double* 
 
 int invalid(const char* msg) { return report_error(ORTH_EINVAL, msg); }
 
+// A tensor's rows as one run of bytes, with the gaps between them, and whether it
+// has none.
+struct Run {
+  uintptr_t at, end;
+  bool flat;
+};
+Run run_of(const void* p, const orth_grad& g, int64_t ld) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p), es = g.dtype == ORTH_BF16 ? 2 : 4;
+  return {at, at + ((uintptr_t)(g.rows - 1) * (uintptr_t)ld + (uintptr_t)g.cols) * es, g.rows == 1 || ld == g.cols};
+}
+// Whether a gradient and its output share bytes without being the same.  Rows
+// of one stride share none if they lie side by side in it.
+bool shares(const orth_grad& g) {
+  if (g.grad == g.out) return false;
+  const Run a = run_of(g.grad, g, g.ld_grad), b = run_of(g.out, g, g.ld_out);
+  if (a.at >= b.end || b.at >= a.end) return false;
+  if (g.ld_grad != g.ld_out || g.rows == 1) return true;
+  const uintptr_t es = g.dtype == ORTH_BF16 ? 2 : 4, ld = (uintptr_t)g.ld_out * es, cols = (uintptr_t)g.cols * es;
+  const uintptr_t d = (a.at < b.at ? b.at - a.at : a.at - b.at) % ld;
+  return d < cols || d + cols > ld;
+}
+
 int validate(const orth_grad* g, int32_t n, bool outs) {
   if (n < 0) return invalid("n must be >= 0");
   if (n > 0 && !g) return invalid("grads is NULL");
@@ -390,13 +412,24 @@ int validate(const orth_grad* g, int32_t n, bool outs) {
       return invalid("leading dimension below the columns");
     if (outs && g[i].grad == g[i].out && g[i].ld_grad != g[i].ld_out)
       return invalid("in place needs equal leading dimensions");
+    // (as in the row-grouped products: past any memory)
+    if ((double)g[i].rows * (double)g[i].ld_grad > 0x1p48 || (outs && (double)g[i].rows * (double)g[i].ld_out > 0x1p48))
+      return invalid("leading dimension too large");
+    if (outs && shares(g[i])) return invalid("an output must be its gradient or apart from it");
   }
   if (outs) {
-    std::vector<const void*> to;
+    std::vector<Run> to;
     for (int i = 0; i < n; ++i)
-      if (g[i].rows && g[i].cols) to.push_back(g[i].out);
-    std::sort(to.begin(), to.end());
-    if (std::adjacent_find(to.begin(), to.end()) != to.end()) return invalid("two outputs are the same");
+      if (g[i].rows && g[i].cols) to.push_back(run_of(g[i].out, g[i], g[i].ld_out));
+    std::sort(to.begin(), to.end(), [](const Run& a, const Run& b) { return a.at < b.at; });
+    // (runs with gaps may lie in each other's)
+    uintptr_t flat_end = 0;
+    for (size_t i = 0; i < to.size(); ++i) {
+      if (i > 0 && to[i].at == to[i - 1].at) return invalid("two outputs are the same");
+      if (!to[i].flat) continue;
+      if (to[i].at < flat_end) return invalid("two outputs overlap");
+      flat_end = to[i].end;
+    }
   }
   return ORTH_OK;
 }

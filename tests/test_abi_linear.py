@@ -210,3 +210,24 @@ def test_too_many_groups(L, groups):
     assert L.orth_linear_grad_weight(a, 1 << 50, 1 << 40, None) == EINVAL
     a = ctypes.byref(linear(groups=2 ** 20))
     assert L.orth_linear_grad_weight_workspace_size(a, ctypes.byref(n)) == OK
+
+
+IN, OUT = 1 << 40, 2 << 40
+
+
+@pytest.mark.parametrize("kw,want", [
+    # (the last of three tensors, 4 x 8 float32: IN + 2^31 and OUT + 2^31 are its places)
+    (dict(out=IN + (2 << 30) + 4), EINVAL), (dict(out=IN + (2 << 30) - 124), EINVAL),
+    (dict(grad=IN, out=IN + 32, ld_grad=16, ld_out=16), OK), (dict(grad=IN, out=IN + 28, ld_grad=16, ld_out=16), EINVAL),
+    (dict(grad=IN + 32, out=IN, ld_grad=16, ld_out=16), OK), (dict(grad=IN, out=IN + 96, ld_grad=16, ld_out=16), OK),
+    (dict(grad=IN, out=IN + 40, ld_grad=16, ld_out=16), EINVAL), (dict(grad=IN, out=IN + 32, ld_grad=16, ld_out=17), EINVAL),
+    (dict(out=OUT + 124), EINVAL), (dict(out=OUT + 128), OK), (dict(out=OUT + (1 << 30) - 4), EINVAL),
+    # rows with gaps may hold another output in them
+    (dict(out=OUT - 32, ld_out=64), OK),
+    (dict(ld_grad=2 ** 47), EINVAL), (dict(ld_out=2 ** 47), EINVAL), (dict(rows=BIG, cols=BIG, ld_grad=2 ** 62, ld_out=2 ** 62), EINVAL)])
+def test_clip_outputs_that_overlap(L, kw, want):
+    """Outputs that share a part of their gradient or of each other.  (A small
+    workspace refuses what is accepted otherwise, before anything is enqueued.)"""
+    o = orth.orth_clip_opts(1.0, 1e-6, 0)
+    rc = L.orth_grad_clip_batched(grads(**kw), 3, ctypes.byref(o), 1 << 45, 1 << 50, 16, None)
+    assert rc == (EWORKSPACE if want == OK else want)
