@@ -28,6 +28,8 @@ CASES = [  # rows, features, classes, scale, classes per piece
     # staged tiles of both edges, aligned and not; dx in slices; dW in slices
     (200, 328, 5003, 2.0, 0), (300, 99, 1500, 1.0, 0), (700, 264, 4000, 1.0, 1504), (2048, 136, 8000, 2.0, 0),
     (1000, 1344, 20001, 2.0, 8192), (6000, 100, 300, 1.0, 0), (4096, 512, 9000, 1.0, 0),
+    # dx on 256-tiles, the last one half full: stored, summed over pieces
+    (4020, 2048, 3001, 1.0, 0), (4020, 2048, 7003, 1.0, 3000),
 ]
 
 
